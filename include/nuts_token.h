@@ -53,6 +53,11 @@ enum {
     NUTS_ACT_GELU = 4      /* z Phi(z), Phi the normal distribution function */
 };
 
+/* Added to `act` of a gradient's arguments: for bf16, dz (dg and du) is rounded
+ * to bf16 for the matrix products, which halves them.  Without it two bf16 parts
+ * hold 16 of its bits, so that the rounding of the outputs is all that shows. */
+enum { NUTS_ROUND_DZ = 256 };
+
 /* Embedding of tokens: out[i] = scale table[ids[i]], i < N, rows of D
  * elements; a row of zeros where ids[i] lies outside [0, V) (a position
  * without a token). */
@@ -112,12 +117,11 @@ int nuts_linear(nuts_handle* h, const nuts_linear_args* a, void* workspace, int6
 
 /* Its gradients for dy: dz = dy act'(z); dx = dz w, dw = dz^T x, dbias =
  * sum over the rows of dz (residual's gradient is dy).  Each output may be
- * NULL; pre may be NULL with NUTS_ACT_NONE.  For bf16 with an activation dz is
- * rounded to bf16 for the two products (not for dbias), in M N K <= 2^27 to two
- * bf16 parts. */
+ * NULL; pre may be NULL with NUTS_ACT_NONE.  For bf16 with an activation the two
+ * products (not dbias) take dz in two bf16 parts, in one with NUTS_ROUND_DZ. */
 typedef struct {
     int32_t dtype;
-    int32_t act;
+    int32_t act;           /* NUTS_ACT_, + NUTS_ROUND_DZ */
     int64_t M, N, K;
     const void* dy;    /* [M][N], row stride lddy */
     int64_t lddy;
@@ -158,11 +162,11 @@ int nuts_gated(nuts_handle* h, const nuts_gated_args* a, void* workspace, int64_
 
 /* Its gradients for dy: dg = dy u act'(g), du = dy act(g); dx = dg wg +
  * du wu, dwg = dg^T x, dwu = du^T x.  dx may be NULL, and dwg and dwu both.
- * For bf16, dg and du are rounded to bf16 for the products, in M F K <= 2^27 to
- * two bf16 parts. */
+ * For bf16 the products take dg and du in two bf16 parts, in one with
+ * NUTS_ROUND_DZ. */
 typedef struct {
     int32_t dtype;
-    int32_t act;
+    int32_t act;       /* NUTS_ACT_, + NUTS_ROUND_DZ */
     int64_t M, F, K;
     const void* dy;    /* [M][F], row stride lddy */
     int64_t lddy;

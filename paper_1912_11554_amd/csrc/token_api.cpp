@@ -148,6 +148,7 @@ hipError_t forward(const Forward& f, Space& space, bool run, hipStream_t stream)
 // dx and dw (and dw2) for dz (and dz2)
 struct Backward {
     int dtype, act;
+    bool rounded;  // bf16: dz in one part
     int64_t M, N, K;
     const void* dy;
     int64_t lddy;
@@ -166,12 +167,10 @@ struct Backward {
     void* dbias;
 };
 // A bf16 dz rounded once adds as much error to its products as their own rounding
-// does (2.3e-3 of their norm in all, where one rounding leaves 1.7e-3).  Up to so
-// many products it is kept in two bf16 matrices instead (16 bits): twice the products,
-// which cost little beside the launches there (linear layer and gated block, one part
-// and two: 128 x 1024 x 1024 16.4 and 19.6 us, 19.7 and 26.5 us; 1024^3 27 and 46 us, 41
-// and 60 us).
-constexpr double kTwoParts = 0x1p27;
+// does (2.3e-3 of their norm in all, where one rounding leaves 1.7e-3).  So it is kept
+// in two bf16 matrices (16 bits), twice the products, unless the caller asks for one
+// (linear layer and gated block, one part and two, us: 128 x 1024 x 1024 16.4 and 19.6,
+// 19.7 and 26.5; 1024^3 27 and 46, 41 and 60).
 const void* part_of(const void* dz, int part, int64_t rest)
 {
     return dz ? (const char*)dz + (part ? rest * 2 : 0) : nullptr;
@@ -184,7 +183,7 @@ hipError_t backward(const Backward& b, Space& space, bool run, hipStream_t strea
     int64_t ldz = b.lddy, rest = 0;
     if (products && !own) {
         ldz = up(b.N, 8);
-        if (b.dtype == NUTS_BF16 && (double)b.M * b.N * b.K <= kTwoParts) rest = b.M * ldz;
+        if (b.dtype == NUTS_BF16 && !b.rounded) rest = b.M * ldz;
         dz = space.take((b.M * ldz + rest) * (int64_t)type_bytes(b.dtype));
         if (b.gated) du = space.take((b.M * ldz + rest) * (int64_t)type_bytes(b.dtype));
     }
@@ -257,14 +256,17 @@ Forward gated_forward(const nuts_gated_args& a)
     f.epi = {a.y, a.ldy, nullptr, nullptr, 0, a.pre, a.act, a.dtype};
     return f;
 }
+// The activation of a gradient's arguments.
+int act_of(int act) { return act & ~NUTS_ROUND_DZ; }
+
 Backward linear_backward(const nuts_linear_grad_args& a)
 {
-    return {a.dtype, a.act, a.M, a.N, a.K, a.dy, a.lddy, a.x, a.ldx, a.w, a.ldw, nullptr, 0, false, a.pre,
+    return {a.dtype, act_of(a.act), (a.act & NUTS_ROUND_DZ) != 0, a.M, a.N, a.K, a.dy, a.lddy, a.x, a.ldx, a.w, a.ldw, nullptr, 0, false, a.pre,
             a.dx, a.lddx, a.dw, nullptr, a.lddw, 0, a.dbias};
 }
 Backward gated_backward(const nuts_gated_grad_args& a)
 {
-    return {a.dtype, a.act, a.M, a.F, a.K, a.dy, a.lddy, a.x, a.ldx, a.wg, a.ldwg, a.wu, a.ldwu, true, a.pre,
+    return {a.dtype, act_of(a.act), (a.act & NUTS_ROUND_DZ) != 0, a.M, a.F, a.K, a.dy, a.lddy, a.x, a.ldx, a.wg, a.ldwg, a.wu, a.ldwu, true, a.pre,
             a.dx, a.lddx, a.dwg, a.dwu, a.lddwg, a.lddwu, nullptr};
 }
 
@@ -310,11 +312,11 @@ int check(Check& c, const nuts_gated_args& a)
 }
 int check(Check& c, const nuts_linear_grad_args& a)
 {
-    check_sizes(c, a.dtype, a.act, a.M, a.N, a.K, "N");
+    check_sizes(c, a.dtype, act_of(a.act), a.M, a.N, a.K, "N");
     const size_t b = type_bytes(a.dtype);
     if (c.code == NUTS_OK) {
         c.matrix("dy", a.dy, a.M, a.N, a.lddy, b);
-        if (a.act != NUTS_ACT_NONE) c.buffer("pre", a.pre, a.M * a.N, 4);
+        if (act_of(a.act) != NUTS_ACT_NONE) c.buffer("pre", a.pre, a.M * a.N, 4);
         if (a.dw) c.matrix("x", a.x, a.M, a.K, a.ldx, b);
         if (a.dx) c.matrix("w", a.w, a.N, a.K, a.ldw, b);
         c.matrix("dx", a.dx, a.M, a.K, a.lddx, b, false);
@@ -325,7 +327,7 @@ int check(Check& c, const nuts_linear_grad_args& a)
 }
 int check(Check& c, const nuts_gated_grad_args& a)
 {
-    check_sizes(c, a.dtype, a.act, a.M, a.F, a.K, "F");
+    check_sizes(c, a.dtype, act_of(a.act), a.M, a.F, a.K, "F");
     const size_t b = type_bytes(a.dtype);
     if (c.code == NUTS_OK) {
         if ((a.dwg == nullptr) != (a.dwu == nullptr) && a.F > 0 && a.K > 0)

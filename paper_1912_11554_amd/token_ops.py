@@ -25,6 +25,7 @@ class _Torch:
 torch = _Torch()
 NUTS_F32, NUTS_BF16 = 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "sigmoid": 2, "silu": 3, "gelu": 4}
+NUTS_ROUND_DZ = 256
 
 _P, _i64, _i32, _dbl = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double
 
@@ -169,17 +170,19 @@ class TokenOps:
             None if pre is None else pre.data_ptr()), x.device)
         return (out, pre) if save else out
 
-    def linear_grad(self, dy, x, w, *, act="none", pre=None, bias=True, dx=True, dw=True):
+    def linear_grad(self, dy, x, w, *, act="none", pre=None, bias=True, dx=True, dw=True, rounded=False):
         """Gradients (dx [M, K], dw [N, K], dbias [N]) of ``linear`` for dy
-        [M, N]; None where not asked for.  The residual's gradient is dy."""
+        [M, N]; None where not asked for.  The residual's gradient is dy.  With
+        bf16 and an activation, rounded=True rounds dy act'(z) to bf16 for the
+        two products: half of their work, and 1.4 times the outputs' error."""
         (M, K), N, t = x.shape, w.shape[0], dy.dtype
         empty = lambda *shape: torch.empty(*shape, dtype=t, device=dy.device)  # noqa: E731
         gx, gw = empty(M, K) if dx else None, empty(N, K) if dw else None
         gb = empty(N) if bias else None
-        code = _act(act)
+        code = _act(act) | (NUTS_ROUND_DZ if rounded else 0)
         if pre is not None:
             pre, _ = _matrix(pre, "pre", torch.float32, M, N) if pre.is_contiguous() else _refuse("pre")
-        elif code:
+        elif act != "none":
             raise ValueError("the gradient through an activation needs pre (linear(..., save=True))")
         self._call("nuts_linear_grad", _LinearGrad(
             _type(dy, "dy"), code, M, N, K, *_matrix(dy, "dy", t, M, N), *_matrix(x, "x", t), *_matrix(w, "w", t, N, K),
@@ -201,9 +204,11 @@ class TokenOps:
             x.device)
         return (out, pre) if save else out
 
-    def gated_grad(self, dy, x, wg, wu, pre, *, act="silu", dx=True, dw=True):
+    def gated_grad(self, dy, x, wg, wu, pre, *, act="silu", dx=True, dw=True, rounded=False):
         """Gradients (dx [M, K], dwg [F, K], dwu [F, K]) of ``gated`` for dy
-        [M, F]; None where not asked for."""
+        [M, F]; None where not asked for.  With bf16, rounded=True rounds the
+        gradients of the two products' results to bf16: half of the work, and
+        1.4 times the outputs' error."""
         (M, K), F, t = x.shape, wg.shape[0], dy.dtype
         empty = lambda *shape: torch.empty(*shape, dtype=t, device=dy.device)  # noqa: E731
         gx = empty(M, K) if dx else None
@@ -212,7 +217,7 @@ class TokenOps:
             _refuse("pre")
         at = lambda g: (None, 0) if g is None else (g.data_ptr(), K)  # noqa: E731
         self._call("nuts_gated_grad", _GatedGrad(
-            _type(dy, "dy"), _act(act), M, F, K, *_matrix(dy, "dy", t, M, F), *_matrix(x, "x", t),
+            _type(dy, "dy"), _act(act) | (NUTS_ROUND_DZ if rounded else 0), M, F, K, *_matrix(dy, "dy", t, M, F), *_matrix(x, "x", t),
             *_matrix(wg, "wg", t, F, K), *_matrix(wu, "wu", t, F, K), pre.data_ptr(), *at(gx), *at(gg), *at(gu)),
             dy.device)
         return gx, gg, gu

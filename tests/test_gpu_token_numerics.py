@@ -1,0 +1,105 @@
+"""Accuracy and ranges of the token-model operators where a bound on every
+element says too little: the error of whole outputs against that of their one
+rounding, relative errors far from zero, infinities and NaN in every kernel of
+the products, launches past one grid."""
+import pytest
+
+from tests.gpu_common import say
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def s():
+    import paper_1912_11554_amd as nuts
+    h = nuts.Sampler(0)
+    yield h
+    h.close()
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _gen(seed):
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return lambda *q, std=1.0, t=torch.float32: (torch.randn(*q, device="cuda", generator=g) * std).to(t)
+
+
+def _act(z, kind):
+    """act(z) and its slope, in z's 64 bits."""
+    torch = _torch()
+    if kind == "none":
+        return z, torch.ones_like(z)
+    if kind == "gelu":
+        cdf = torch.special.ndtr(z)
+        return z * cdf, cdf + z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    p, q = torch.special.expit(z), torch.special.expit(-z)
+    return (p, p * q) if kind == "sigmoid" else (z * p, p + z * p * q)
+
+
+# --------------------------------------------------------------------------
+# bf16 gradients.  With d = dy act'(z) in two parts, at most 2^-17 |d| is left
+# out, and fp32 sums of up to n products add n 2^-24: next to the rounding of
+# the output (1.7e-3 of its norm) both vanish, so an output's error is that
+# rounding's, to a hundredth.  Rounded to bf16, d's error is as large again and
+# independent: 1.4 times in all.
+
+def _errors(got, ref):
+    """Norm of got's error, in units of that of ref rounded once."""
+    once = (ref.bfloat16().double() - ref).norm()
+    return float((got.double() - ref).norm() / once)
+
+
+BF16_SHAPES = [(200, 264, 136), (130, 520, 264), (520, 1032, 512), (1100, 1040, 200), (2050, 1032, 520)]
+
+
+@pytest.mark.parametrize("shape", BF16_SHAPES)
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "gelu"])
+def test_bf16_linear_gradients_round_once(s, shape, act):
+    torch = _torch()
+    M, N, K = shape
+    say("one rounding, linear", shape, act)
+    rand, bf = _gen(M + N + K), torch.bfloat16
+    x, w, dy = rand(M, K, t=bf), rand(N, K, std=K ** -0.5, t=bf), rand(M, N, t=bf)
+    _, pre = s.linear(x, w, act=act, save=True)
+    d = dy.double() * _act(pre.double(), act)[1]
+    refs = d @ w.double(), d.T @ x.double()
+    for got, ref in zip(s.linear_grad(dy, x, w, act=act, pre=pre), refs):
+        assert _errors(got, ref) <= 1.01
+    for got, ref in zip(s.linear_grad(dy, x, w, act=act, pre=pre, rounded=True), refs):
+        assert 1.2 <= _errors(got, ref) <= 1.6
+
+
+@pytest.mark.parametrize("shape", BF16_SHAPES)
+def test_bf16_gated_gradients_round_once(s, shape):
+    torch = _torch()
+    M, F, K = shape
+    say("one rounding, gated", shape)
+    rand, bf = _gen(M + F + K + 1), torch.bfloat16
+    x, dy = rand(M, K, t=bf), rand(M, F, t=bf)
+    wg, wu = rand(F, K, std=K ** -0.5, t=bf), rand(F, K, std=K ** -0.5, t=bf)
+    _, pre = s.gated(x, wg, wu, save=True)
+    a, slope = _act(pre[0].double(), "silu")
+    dg, du = dy.double() * pre[1].double() * slope, dy.double() * a
+    refs = dg @ wg.double() + du @ wu.double(), dg.T @ x.double(), du.T @ x.double()
+    for got, ref in zip(s.gated_grad(dy, x, wg, wu, pre), refs):
+        assert _errors(got, ref) <= 1.01
+    for got, ref in zip(s.gated_grad(dy, x, wg, wu, pre, rounded=True), refs):
+        assert 1.2 <= _errors(got, ref) <= 1.6
+
+
+def test_rounding_is_the_identity_where_nothing_is_rounded(s):
+    # fp32, and bf16 without an activation
+    torch = _torch()
+    say("rounded, no effect")
+    rand = _gen(9)
+    for t, act in ((torch.float32, "silu"), (torch.bfloat16, "none")):
+        x, w, dy = rand(70, 40, t=t), rand(50, 40, t=t), rand(70, 50, t=t)
+        _, pre = s.linear(x, w, act=act, save=True)
+        a, b = (s.linear_grad(dy, x, w, act=act, pre=pre, rounded=r) for r in (False, True))
+        assert all(torch.equal(p, q) for p, q in zip(a, b))

@@ -70,3 +70,19 @@ def test_workspace_sizes():
     assert L.nuts_linear_workspace(ctypes.byref(a)) == 0
     a = ops._Linear(2, 0, 100, 128, 1 << 16, p, 1 << 16, p, 1 << 16, None, None, 0, p, 128, None)
     assert L.nuts_linear_workspace(ctypes.byref(a)) > 0
+
+
+def test_rounding_is_a_gradients_choice():
+    # NUTS_ROUND_DZ halves the matrices of a bf16 gradient, at any size; it is no activation
+    L = nuts.load_library()
+    assert ops.NUTS_ROUND_DZ == int(re.search(r"NUTS_ROUND_DZ = (\d+)", _source()).group(1))
+    p, silu = 1 << 20, ops.ACTIVATIONS["silu"]
+    for M, N, K in ((64, 64, 64), (4096, 4096, 4096)):
+        need = [L.nuts_linear_grad_workspace(ctypes.byref(ops._LinearGrad(
+            2, silu + flag, M, N, K, p, N, p, K, p, K, p, p, K, None, 0, None))) for flag in (0, ops.NUTS_ROUND_DZ)]
+        assert need[0] == 2 * M * N * 2 and need[1] == M * N * 2
+    for flag in (ops.NUTS_ROUND_DZ, 512):
+        a = ops._Linear(2, silu + flag, 64, 64, 64, p, 64, p, 64, None, None, 0, p, 64, None)
+        assert L.nuts_linear_workspace(ctypes.byref(a)) == nuts.NUTS_EINVAL
+    a = ops._LinearGrad(2, silu + 512, 64, 64, 64, p, 64, p, 64, p, 64, p, p, 64, None, 0, None)
+    assert L.nuts_linear_grad_workspace(ctypes.byref(a)) == nuts.NUTS_EINVAL
