@@ -26,6 +26,7 @@ struct KernelArgs {
     int K;
     int steps;        // stages of one term
     int nterms;
+    int small_stages; // so many stages at the start are of terms of corrections
     int tiles_m, tiles_n;
     int slices;       // the stages of all terms in so many runs (split sums)
     int64_t ldp;
@@ -140,7 +141,8 @@ __device__ __forceinline__ int gated_row(int at)
 // or a product leaves the fp32 range, the leading products (at least 64 times
 // the corrections) hold the infinity or NaN that the fp32 product has, and the
 // corrections hold inf - inf and inf * 0: a NaN becomes -2^122 here, which no
-// infinity and no NaN notices, nor in the sum of kMaxSlices slices.
+// infinity and no NaN notices, nor in the sum of kMaxSlices slices.  Corrections are
+// the lower parts of fp32 factors and the terms of a bf16 dz's second part.
 __device__ __forceinline__ v4f finite(v4f c)
 {
     constexpr float big = 0x1p122f;
@@ -321,6 +323,13 @@ __device__ __forceinline__ Run run_of(const ConstArgs& p)
     const int64_t all = (int64_t)p.steps * p.nterms;
     return {(int)(all * blockIdx.y / p.slices), (int)(all * (blockIdx.y + 1) / p.slices)};
 }
+// The run's stage, counted from one, after which its sums are of corrections alone and
+// done with them (0: it has none).
+__device__ __forceinline__ int small_end(const ConstArgs& p, Run run)
+{
+    const int end = p.small_stages < run.to ? p.small_stages : run.to;
+    return end > run.from ? end - run.from : 0;
+}
 
 // ---------------------------------------------------------------------------
 // bf16 operands of 16-byte aligned rows of a whole multiple of 8 elements,
@@ -466,7 +475,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_kernel(KernelArgs)
     static_assert(kGroups % kRing == 0 && kAhead < kRing, "the ring goes round a whole number of times a stage");
     static_assert(kStep == 64 && kGroups - kAhead >= FM, "the first half's columns are done with when the waves meet");
     v8bf fa[kRing], fb[2][FN];
-    const int stages = run.to - run.from;
+    const int stages = run.to - run.from, small = small_end(p, run);
     if (stages > 0) {
         offsets();
         copy_stage(0);
@@ -508,6 +517,12 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void product_kernel(KernelArgs)
             for (int j = 0; j < FN; ++j)
                 acc[g % FM][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[kk][j], fa[g % kRing], acc[g % FM][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if (s + 1 == small) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = finite(acc[i][j]);
         }
     }
     __syncthreads();
@@ -674,6 +689,7 @@ __global__ __launch_bounds__(256, B > 64 ? 2 : 3) void staged_kernel(KernelArgs)
 #pragma unroll
     for (int h = 0; h < AHEAD; ++h)
         if (run.from + h < run.to) fetch_stage(pieces[h]);
+    const int small = small_end(p, run);
     for (int s = run.from; s < run.to; s += AHEAD) {
 #pragma unroll
         for (int h = 0; h < AHEAD; ++h) {
@@ -706,6 +722,12 @@ __global__ __launch_bounds__(256, B > 64 ? 2 : 3) void staged_kernel(KernelArgs)
                         }
                     }
                 }
+            }
+            if (PARTS == 1 && s + h + 1 - run.from == small) {
+#pragma unroll
+                for (int i = 0; i < F; ++i)
+#pragma unroll
+                    for (int j = 0; j < F; ++j) acc[i][j] = finite(acc[i][j]);
             }
             __syncthreads();
         }
@@ -824,6 +846,7 @@ hipError_t launch_product(const Product& p, float* partials, int num_cu, hipStre
     a.K = (int)p.K;
     a.steps = (int)steps_of(p);
     a.nterms = p.nterms;
+    a.small_stages = p.small_terms * a.steps;
     a.slices = plan.slices;
     a.ldp = up(p.N, 4);
     a.partials = partials;

@@ -47,6 +47,7 @@ struct Product {
     bool b_rows;      // B is stored [k][n] (with a_rows, always)
     bool gated;       // two sums per output: act(A B^T) (A B2^T)
     int nterms;
+    int small_terms;  // so many terms at the start are corrections of the others
     int sets;         // products of one shape in one launch: set s has terms[s]
     Term terms[2][kMaxTerms];
     Epilogue epi[2];

@@ -203,6 +203,7 @@ hipError_t backward(const Backward& b, Space& space, bool run, hipStream_t strea
     p.b_rows = true;
     p.epi[0].dtype = p.epi[1].dtype = b.dtype;
     const bool dz_direct = direct(dz, b.N, ldz, b.dtype);
+    const int parts = rest ? 2 : 1;
     if (b.dx && b.M > 0 && b.K > 0) {
         p.M = b.M;
         p.N = b.K;
@@ -210,7 +211,8 @@ hipError_t backward(const Backward& b, Space& space, bool run, hipStream_t strea
         p.staged = !dz_direct || !direct(b.w, b.K, b.ldw, b.dtype) || (b.gated && !direct(b.w2, b.K, b.ldw2, b.dtype));
         p.sets = 1;
         p.nterms = 0;
-        for (int part = 0; part < (rest ? 2 : 1); ++part) {
+        p.small_terms = (parts - 1) * (b.gated ? 2 : 1);
+        for (int part = parts - 1; part >= 0; --part) {
             p.terms[0][p.nterms++] = {part_of(dz, part, rest), b.w, nullptr, ldz, b.ldw, 0};
             if (b.gated) p.terms[0][p.nterms++] = {part_of(du, part, rest), b.w2, nullptr, ldz, b.ldw2, 0};
         }
@@ -228,11 +230,12 @@ hipError_t backward(const Backward& b, Space& space, bool run, hipStream_t strea
         p.K = b.M;
         p.staged = !dz_direct || !direct(b.x, b.K, b.ldx, b.dtype);
         p.a_rows = true;
-        p.nterms = rest ? 2 : 1;
+        p.nterms = parts;
+        p.small_terms = parts - 1;
         p.sets = b.gated ? 2 : 1;
-        for (int part = 0; part < p.nterms; ++part) {
-            p.terms[0][part] = {part_of(dz, part, rest), b.x, nullptr, ldz, b.ldx, 0};
-            p.terms[1][part] = {part_of(du, part, rest), b.x, nullptr, ldz, b.ldx, 0};
+        for (int t = 0; t < parts; ++t) {
+            p.terms[0][t] = {part_of(dz, parts - 1 - t, rest), b.x, nullptr, ldz, b.ldx, 0};
+            p.terms[1][t] = {part_of(du, parts - 1 - t, rest), b.x, nullptr, ldz, b.ldx, 0};
         }
         p.epi[0].out = b.dw;
         p.epi[0].ldo = b.lddw;

@@ -103,3 +103,59 @@ def test_rounding_is_the_identity_where_nothing_is_rounded(s):
         _, pre = s.linear(x, w, act=act, save=True)
         a, b = (s.linear_grad(dy, x, w, act=act, pre=pre, rounded=r) for r in (False, True))
         assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# --------------------------------------------------------------------------
+# Infinities and NaN.  Where an output's sum holds none, it is bit for bit what
+# it is without them elsewhere; where it does, it is what the sum in 64 bits
+# gives: NaN, or the same infinity.
+
+def _same_limits(got, ref, clean, touched, what):
+    torch = _torch()
+    ref = ref.to(got.dtype)
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)), f"{what}: NaN"
+    inf = torch.isinf(ref)
+    assert torch.equal(torch.isinf(got), inf) and torch.equal(got[inf], ref[inf]), f"{what}: infinities"
+    assert torch.equal(got[~touched], clean[~touched]), f"{what}: elsewhere"
+    assert inf.any() and torch.isfinite(got).any(), what  # (the case has both)
+
+
+def _touched(shape, rows, cols):
+    t = _torch().zeros(shape, dtype=_torch().bool, device="cuda")
+    t[rows] = True
+    t[:, cols] = True
+    return t
+
+
+# M, N, K: 64 x 64 tiles on and off the 16-byte grid, with slices, 128 x 128, 256 x 256
+PRODUCT_SHAPES = [(70, 40, 96), (300, 75, 137), (130, 128, 4096), (130, 100, 4099), (2560, 2600, 72), (3600, 3640, 72)]
+
+
+@pytest.mark.parametrize("shape", PRODUCT_SHAPES)
+@pytest.mark.parametrize("rounded", [False, True])
+def test_infinite_factors_of_bf16_gradients(s, shape, rounded):
+    # dz's second part times an infinity is an infinity of either sign, or 0 * inf
+    torch = _torch()
+    M, N, K = shape
+    say("infinite factors", shape, rounded)
+    rand, bf = _gen(M + N), torch.bfloat16
+    x, w, dy = rand(M, K, t=bf), rand(N, K, t=bf), rand(M, N, t=bf)
+    z = rand(M, N)
+    clean = s.linear_grad(dy, x, w, act="silu", pre=z, rounded=rounded)
+    x[5, 3], x[6, 7], w[9, 11], w[10, 13] = float("inf"), float("-inf"), float("-inf"), float("inf")
+    dx, dw, db = s.linear_grad(dy, x, w, act="silu", pre=z, rounded=rounded)
+    d = dy.double() * _act(z.double(), "silu")[1]
+    _same_limits(dx, d @ w.double(), clean[0], _touched((M, K), [], [11, 13]), "dx")
+    _same_limits(dw, d.T @ x.double(), clean[1], _touched((N, K), [], [3, 7]), "dw")
+    assert torch.equal(db, clean[2])
+    # the gated block: two products each with parts of their own
+    x, w2, pre = rand(M, K, t=bf), rand(N, K, t=bf), rand(2, M, N)
+    w = rand(N, K, t=bf)
+    clean = s.gated_grad(dy, x, w, w2, pre, rounded=rounded)
+    x[5, 3], w[9, 11], w2[10, 13] = float("inf"), float("-inf"), float("inf")
+    got = s.gated_grad(dy, x, w, w2, pre, rounded=rounded)
+    a, slope = _act(pre[0].double(), "silu")
+    dg, du = dy.double() * pre[1].double() * slope, dy.double() * a
+    _same_limits(got[0], dg @ w.double() + du @ w2.double(), clean[0], _touched((M, K), [], [11, 13]), "dx")
+    _same_limits(got[1], dg.T @ x.double(), clean[1], _touched((N, K), [], [3]), "dwg")
+    _same_limits(got[2], du.T @ x.double(), clean[2], _touched((N, K), [], [3]), "dwu")
