@@ -133,10 +133,14 @@ __device__ __forceinline__ void activate_slope(float z, int act, float* a, float
 // The three bf16 parts of fp32 values, cut off rather than rounded: eight of the
 // 24 bits each, so the parts hold the value exactly (down to bf16's least
 // magnitude, 2^-133) and no finite value leaves the range.  An infinity's other
-// parts are NaN, which the products' corrections drop.  out[p]: part p of two
-// values, the first in the low half.
+// parts are NaN, which the products' corrections drop.  A NaN is made quiet first: a
+// signalling one may have all of its set bits in the half that is cut off, where the
+// first part would be an infinity.  out[p]: part p of two values, the first in the
+// low half.
 __device__ __forceinline__ void parts3(float x, float y, uint32_t (&out)[3])
 {
+    x = __builtin_canonicalizef(x);
+    y = __builtin_canonicalizef(y);
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
         const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);

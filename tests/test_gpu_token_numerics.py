@@ -159,3 +159,71 @@ def test_infinite_factors_of_bf16_gradients(s, shape, rounded):
     _same_limits(got[0], dg @ w.double() + du @ w2.double(), clean[0], _touched((M, K), [], [11, 13]), "dx")
     _same_limits(got[1], dg.T @ x.double(), clean[1], _touched((N, K), [], [3]), "dwg")
     _same_limits(got[2], du.T @ x.double(), clean[2], _touched((N, K), [], [3]), "dwu")
+
+
+def _plant(t):
+    """Infinities, and a NaN whose set bits all lie in the lower half in fp32,
+    in a matrix; (rows, columns) that they touch."""
+    torch = _torch()
+    t[3, 5], t[8, 2] = float("inf"), float("-inf")
+    if t.dtype == torch.float32:
+        t.view(torch.int32)[11, 7] = 0x7f800001
+    else:
+        t[11, 7] = float("nan")
+    return [3, 8, 11], [5, 2, 7]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("shape", [(2, 40, 96), (40, 40, 96)] + PRODUCT_SHAPES)
+def test_infinities_and_nan_in_every_product(s, shape, dtype):
+    torch = _torch()
+    M, N, K = shape
+    say("infinities", shape, dtype)
+    rand, t = _gen(M + N + 7), getattr(torch, dtype)
+    x, w, w2, dy = rand(M, K, t=t), rand(N, K, t=t), rand(N, K, t=t), rand(M, N, t=t)
+    none = []
+    # forward: w's touch whole columns, x's whole rows
+    y0, g0 = s.linear(x, w), s.gated(x, w, w2, act="none")
+    wrows, wcols = _plant(w)
+    xrows = none
+    if M > 11:
+        xrows, _ = _plant(x)
+    y = x.double() @ w.double().T
+    _same_limits(s.linear(x, w), y, y0, _touched((M, N), xrows, wrows), "y")
+    # (an infinite product may meet a finite one of either sign, so NaN comes of it as 0 inf does)
+    _same_limits(s.gated(x, w, w2, act="none"), y * (x.double() @ w2.double().T), g0, _touched((M, N), xrows, wrows), "gated")
+    # gradients: w's columns are dx's, x's columns dw's, dy's rows dx's and its columns dw's
+    clean = s.linear_grad(dy, rand(M, K, t=t), rand(N, K, t=t))
+    x, w = rand(M, K, t=t), rand(N, K, t=t)
+    clean = s.linear_grad(dy, x, w)
+    _plant(w)
+    dx, dw, db = s.linear_grad(dy, x, w)
+    _same_limits(dx, dy.double() @ w.double(), clean[0], _touched((M, K), none, wcols), "dx")
+    assert torch.equal(dw, clean[1])
+    if M > 11:
+        w = rand(N, K, t=t)
+        clean = s.linear_grad(dy, x, w)
+        dyrows, dycols = _plant(dy)
+        dx, dw, db = s.linear_grad(dy, x, w)
+        _same_limits(dx, dy.double() @ w.double(), clean[0], _touched((M, K), dyrows, none), "dx")
+        _same_limits(dw, dy.double().T @ x.double(), clean[1], _touched((N, K), dycols, none), "dw")
+        _same_limits(db, dy.double().sum(0), clean[2], _touched((1, N), none, dycols)[0], "dbias")
+
+
+@pytest.mark.parametrize("shape", [(2, 40, 96)] + PRODUCT_SHAPES)
+def test_values_at_the_top_of_the_fp32_range(s, shape):
+    # the largest value times 1/2 and 2, and sums that the corrections reach the top of
+    torch = _torch()
+    M, N, K = shape
+    say("top of the range", shape)
+    rand = _gen(M + N + 8)
+    x, w = rand(M, K), rand(N, K)
+    big = torch.finfo(torch.float32).max
+    x[:, 0] = 0
+    x[1, 0] = big
+    w[0::2, 0], w[1::2, 0] = 0.5, 2.0
+    clean = s.linear(x, w)[:1]
+    y = s.linear(x, w)
+    assert (y[1, 0::2].double() / (big / 2) - 1).abs().max() <= 4 * U
+    assert (y[1, 1::2] == float("inf")).all()
+    assert torch.equal(y[:1], clean) and torch.isfinite(y[2:]).all()
