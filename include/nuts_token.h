@@ -24,8 +24,9 @@
  *   - Arithmetic is fp32 or wider, rounded once on output.  bf16 matrix
  *     products run on the bf16 matrix cores with fp32 sums; fp32 ones either on
  *     the fp32 matrix cores (up to 64 rows of x) or as three bf16 parts a factor
- *     (products of relative size 2^-22 and below left out).  Infinities and
- *     NaN come out as in fp32 products.
+ *     (products of relative size 2^-22 and below left out; a factor to multiples
+ *     of 2^-133, so below 2^-110 it has fewer digits and below 2^-133 it is zero).
+ *     Infinities and NaN come out as in fp32 products of these factors.
  *   - Where a function nuts_..._workspace exists, the call needs that many
  *     bytes of device memory, 16-byte aligned, in `workspace` (NUTS_EINVAL if
  *     fewer are given); the size is a function of the arguments alone, zero in

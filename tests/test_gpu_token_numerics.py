@@ -227,3 +227,18 @@ def test_values_at_the_top_of_the_fp32_range(s, shape):
     assert (y[1, 0::2].double() / (big / 2) - 1).abs().max() <= 4 * U
     assert (y[1, 1::2] == float("inf")).all()
     assert torch.equal(y[:1], clean) and torch.isfinite(y[2:]).all()
+
+
+@pytest.mark.parametrize("M", [3, 130])
+@pytest.mark.parametrize("e", [-105, -120, -130, -149])
+def test_small_fp32_factors(s, M, e):
+    # tiles take a factor to multiples of 2^-133, few rows to fp32's own
+    torch = _torch()
+    say("small factors", M, e)
+    K = 64
+    rand = _gen(M - e)
+    x = ((rand(M, K).abs() + 1).double() * 2.0 ** e).float()
+    w = rand(40, K) * 2.0 ** 100
+    ref, size = x.double() @ w.double().T, x.double() @ w.double().abs().T
+    off = 2.0 ** -133 * w.double().abs().sum(1) if M > 64 else 0
+    assert ((s.linear(x, w).double() - ref).abs() <= (K + 8) * U * size + off).all()
