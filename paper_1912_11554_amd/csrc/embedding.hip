@@ -13,11 +13,6 @@ namespace nuts {
 namespace token {
 namespace {
 
-// A launch has at most 2^22 workgroups of 256 (a grid holds fewer than 2^32
-// threads), each of which takes further blocks of the work in turn.
-constexpr int64_t kMaxGroups = (int64_t)1 << 22;
-unsigned groups_of(int64_t blocks) { return (unsigned)(blocks < kMaxGroups ? blocks : kMaxGroups); }
-
 // A run of W elements of a row: 16 bytes, or one element where a row is shorter
 // than that.  The last run of a row ends with the row and so overlaps the one
 // before it; both compute and write the same values there.
@@ -135,13 +130,6 @@ __device__ __forceinline__ Same same_digit(uint32_t digit, int bits, uint64_t li
         hi &= ~((uint32_t)(v >> 32) ^ mine);
     }
     return {lo, hi};
-}
-
-// Orders the lanes' LDS accesses before it against those after it.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
 }
 
 // Positions that one workgroup sorts in LDS: one launch for four or more.  A table's

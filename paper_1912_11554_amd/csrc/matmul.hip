@@ -47,11 +47,6 @@ __device__ __forceinline__ Epilogue epilogue_of(const ConstArgs& p, int set)
     return {q.out, q.ldo, q.bias, q.res, q.ldr, q.pre, q.act, q.dtype};
 }
 
-// A launch of the passes below has at most 2^22 workgroups (a grid holds fewer
-// than 2^32 threads), each of which takes further blocks of the work in turn.
-constexpr int64_t kMaxGroups = (int64_t)1 << 22;
-unsigned groups_of(int64_t blocks) { return (unsigned)(blocks < kMaxGroups ? blocks : kMaxGroups); }
-
 // ---------------------------------------------------------------------------
 // Copies to LDS.  The destination is the wave's LDS address in m0 plus 16 bytes
 // a lane; the address is a uniform base plus 32 bits a lane.  Issued without
@@ -226,13 +221,6 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t M, int64_t N, 
         for (int i = 0; i < W; ++i) z[i] += r[i];
     }
     store_run<W>(e.out, e.dtype, m * e.ldo + n, count, z);
-}
-
-// Orders the lanes' LDS accesses before it against those after it.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
 }
 
 // A wave's rectangle of C through LDS, AT blocks of 16 rows at a time: a lane
@@ -995,7 +983,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(FewRows p)
 template <typename T, bool GATED>
 void run_few_rows(const FewRows& p, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)((p.N + 15) / 16);
+    const unsigned grid = (unsigned)((p.N + 15) / 16);  // (N is below 2^23, as the stride of y)
     // 16 waves have the loads in flight that 8 with two factors have (bf16, one row by
     // 4096 x 4096: 9.5 us, 11.4 with 8 waves; gated, 4 by 14,336 x 4096: 46.7 us
     // with 8, 48.1 with 16)
@@ -1035,13 +1023,16 @@ namespace {
 // gated block's 110 (117).
 int64_t slope_rows(int64_t M, int64_t N, bool sums) { return sums && M * N >= (int64_t)1 << 22 ? 16 : 4; }
 
+// (Past one row of the grid the work goes on in the next: a loop over it costs 7%, this 2.)
 template <int ROWS, bool GATED>
-__global__ __launch_bounds__(256) void slope_kernel(Slope s, int64_t stripes)
+__global__ __launch_bounds__(256) void slope_kernel(Slope s, int64_t stripes, int64_t all)
 {
     constexpr int kEach = ROWS / 4;
     __shared__ float sum[4][64][9];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t stripe = blockIdx.x % stripes, block = blockIdx.x / stripes;
+    const int64_t b = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (b >= all) return;
+    const int64_t stripe = b % stripes, block = b / stripes;
     const int64_t c = (stripe * 64 + lane) * 8;
     const int64_t r0 = block * ROWS + wave * kEach;
     const int count = s.N - c < 8 ? (int)(s.N - c) : 8;  // (none below 1)
@@ -1113,18 +1104,22 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* sums, int64_t b
 {
     __shared__ float part[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t n = (int64_t)blockIdx.x * 64 + lane;
-    float t = 0.0f;
-    if (n < N) {
+    for (int64_t n0 = (int64_t)blockIdx.x * 64; n0 < N; n0 += (int64_t)gridDim.x * 64) {
+        const int64_t n = n0 + lane;
+        float t = 0.0f;
+        if (n < N) {
 #pragma unroll 4
-        for (int64_t b = wave; b < blocks; b += 16) t += sums[b * N + n];
-    }
-    part[wave][lane] = t;
-    __syncthreads();
-    if (wave != 0 || n >= N) return;
+            for (int64_t b = wave; b < blocks; b += 16) t += sums[b * N + n];
+        }
+        part[wave][lane] = t;
+        __syncthreads();
+        if (wave == 0 && n < N) {
 #pragma unroll
-    for (int w = 1; w < 16; ++w) t += part[w][lane];
-    store_f32(dbias, dtype, n, t);
+            for (int w = 1; w < 16; ++w) t += part[w][lane];
+            store_f32(dbias, dtype, n, t);
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace
@@ -1139,13 +1134,15 @@ hipError_t launch_slope(const Slope& s, hipStream_t stream)
 {
     const int64_t rows = slope_rows(s.M, s.N, s.dbias);
     const int64_t stripes = (s.N + 511) / 512, blocks = (s.M + rows - 1) / rows;
-    if (stripes * blocks) {
-        auto go = [&](auto* k) { k<<<(unsigned)(stripes * blocks), 256, 0, stream>>>(s, stripes); };
+    if (const int64_t all = stripes * blocks) {
+        const unsigned row = groups_of(all);
+        const dim3 grid(row, (unsigned)((all + row - 1) / row));
+        auto go = [&](auto* k) { k<<<grid, 256, 0, stream>>>(s, stripes, all); };
         s.gated ? go(slope_kernel<4, true>) : rows == 4 ? go(slope_kernel<4, false>) : go(slope_kernel<16, false>);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (s.dbias && s.N) {
-        bias_kernel<<<(unsigned)((s.N + 63) / 64), 1024, 0, stream>>>(s.sums, blocks, s.N, s.dbias, s.dtype);
+        bias_kernel<<<groups_of((s.N + 63) / 64, 1024), 1024, 0, stream>>>(s.sums, blocks, s.N, s.dbias, s.dtype);
         return hipGetLastError();
     }
     return hipSuccess;

@@ -12,6 +12,13 @@ namespace nuts {
 namespace token {
 
 inline size_t type_bytes(int dtype) { return dtype == NUTS_BF16 ? 2 : 4; }
+// Workgroups of a launch: 2^30 threads at most (a grid holds fewer than 2^32), each
+// workgroup takes further blocks of the work in turn.
+inline unsigned groups_of(int64_t blocks, int threads = 256)
+{
+    const int64_t most = ((int64_t)1 << 30) / threads;
+    return (unsigned)(blocks < most ? blocks : most);
+}
 inline int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // ---------------------------------------------------------------------------

@@ -68,6 +68,13 @@ __device__ __forceinline__ T from_f32(float x)
     return (T)x;  // rounds to nearest even
 }
 
+// Orders the lanes' LDS accesses before it against those after it.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Element i of an array of either type.
 __device__ __forceinline__ float load_as_f32(const void* p, int dtype, int64_t i)
 {

@@ -242,3 +242,44 @@ def test_small_fp32_factors(s, M, e):
     ref, size = x.double() @ w.double().T, x.double() @ w.double().abs().T
     off = 2.0 ** -133 * w.double().abs().sum(1) if M > 64 else 0
     assert ((s.linear(x, w).double() - ref).abs() <= (K + 8) * U * size + off).all()
+
+
+# --------------------------------------------------------------------------
+# More blocks of work than one launch has workgroups.
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_gradients_over_very_many_rows(s, dtype):
+    # 2^26 rows and a few; whole numbers, so every sum is exact in any order
+    torch = _torch()
+    M, t = (1 << 26) + 35, getattr(torch, dtype)
+    say("very many rows", dtype)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    sign = lambda *q, t=t: (torch.randint(0, 2, q, device="cuda", generator=g, dtype=torch.int8) * 2 - 1).to(t)  # noqa: E731
+    x, dy, z = sign(M, 1), sign(M, 1), sign(M, 1, t=torch.float32)
+    w = torch.tensor([[3.0]], device="cuda", dtype=t)
+    dz = torch.where(z > 0, dy, torch.zeros_like(dy))
+    total = dz.sum(dtype=torch.float64)
+    for bias in (True, False):
+        dx, dw, db = s.linear_grad(dy, x, w, act="relu", pre=z, bias=bias)
+        assert torch.equal(dx, 3 * dz)
+        assert float(dw) == float((dz * x).sum(dtype=torch.float64).to(t))
+        if bias:
+            assert float(db) == float(total.to(t))
+    pre = sign(2, M, 1, t=torch.float32)
+    dx, dwg, dwu = s.gated_grad(dy, x, w, -w, pre, act="relu")
+    on = (pre[0] > 0).to(t)
+    dg, du = dy * on * pre[1].to(t), dy * on
+    assert torch.equal(dx, 3 * dg - 3 * du)
+    assert float(dwg) == float((dg * x).sum(dtype=torch.float64).to(t))
+    assert float(dwu) == float((du * x).sum(dtype=torch.float64).to(t))
+
+
+def test_bias_gradient_of_no_rows_by_very_many_columns(s):
+    torch = _torch()
+    N = (1 << 28) + 70
+    say("no rows", N)
+    e = torch.empty
+    bf = torch.bfloat16
+    db = s.linear_grad(e(0, N, dtype=bf, device="cuda"), e(0, 0, dtype=bf, device="cuda"),
+                       e(N, 0, dtype=bf, device="cuda"), dx=False, dw=False)[2]
+    assert db.shape == (N,) and not db.any()
