@@ -79,7 +79,8 @@ def _type(t, name):
 
 
 def _matrix(t, name, dtype, rows=None, cols=None):
-    """(pointer, row stride) of a 2-D tensor with unit column stride."""
+    """(pointer, row stride) of a 2-D tensor with unit column stride (of a
+    single row: its length, whatever the tensor says)."""
     if t.dim() != 2 or t.dtype != dtype:
         raise TypeError(f"{name} must be a 2-D {dtype} tensor, got {t.dim()}-D {t.dtype}")
     R, C = t.shape
@@ -88,7 +89,7 @@ def _matrix(t, name, dtype, rows=None, cols=None):
     ld, step = t.stride()
     if C > 1 and step != 1:
         raise ValueError(f"{name}: columns must be adjacent in memory (strides {t.stride()})")
-    return t.data_ptr(), (ld if R > 1 else max(ld, C))
+    return t.data_ptr(), (ld if R > 1 else C)
 
 
 def _vector(t, name, dtype, n):

@@ -283,3 +283,25 @@ def test_bias_gradient_of_no_rows_by_very_many_columns(s):
     db = s.linear_grad(e(0, N, dtype=bf, device="cuda"), e(0, 0, dtype=bf, device="cuda"),
                        e(N, 0, dtype=bf, device="cuda"), dx=False, dw=False)[2]
     assert db.shape == (N,) and not db.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_a_single_row_of_a_larger_tensor(s, dtype):
+    # the last position of a sequence: a stride of 2^23 elements that nothing goes along
+    torch = _torch()
+    say("one row", dtype)
+    t = getattr(torch, dtype)
+    rand = _gen(12)
+    T, D, N = 1 << 16, 128, 72
+    x = torch.zeros(1, T, D, dtype=t, device="cuda")
+    x[:, -1] = rand(1, D, t=t)
+    row, w, u = x[:, -1], rand(N, D, t=t), rand(N, D, t=t)
+    assert row.shape == (1, D) and row.stride(0) == 1 << 23
+    one = row.clone()
+    assert torch.equal(s.linear(row, w), s.linear(one, w))
+    assert torch.equal(s.gated(row, w, u), s.gated(one, w, u))
+    assert torch.equal(s.linear(row, rand(D, D, t=t) * 0, residual=row), one)
+    _, pre = s.linear(one, w, act="silu", save=True)
+    dy = rand(1, N, t=t)
+    for a, b in zip(s.linear_grad(dy, row, w, act="silu", pre=pre), s.linear_grad(dy, one, w, act="silu", pre=pre)):
+        assert torch.equal(a, b)
