@@ -53,7 +53,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void categorical_kernel(nuts
     constexpr int kWaves = TPR < 64 ? 1 : TPR / 64;
     __shared__ Pair shared[kWaves];
     const int t = threadIdx.x % TPR;
-    const int64_t i = (int64_t)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t i = block * (kThreads / TPR) + threadIdx.x / TPR;
     if (i >= a.M) return;  // (with several waves a row, a workgroup has one row)
     const int64_t target = a.targets[i];
     const T* in = (const T*)a.logits + i * a.ld_logits;
@@ -178,15 +179,21 @@ hipError_t launch(const nuts_categorical_args& a, hipStream_t stream)
 {
     constexpr int64_t E = 16 / sizeof(T);
     const int64_t pieces = a.V / E;
-    const unsigned rows = (unsigned)a.M;
-    if (pieces <= 32) categorical_kernel<T, 16, 2><<<(rows + 15) / 16, 256, 0, stream>>>(a);
-    else if (pieces <= 64) categorical_kernel<T, 32, 2><<<(rows + 7) / 8, 256, 0, stream>>>(a);
-    else if (pieces <= 256) categorical_kernel<T, 64, 4><<<(rows + 3) / 4, 256, 0, stream>>>(a);
-    else if (pieces <= 1024) categorical_kernel<T, 256, 4><<<rows, 256, 0, stream>>>(a);
-    else if (pieces <= 2048) categorical_kernel<T, 256, 16><<<rows, 256, 0, stream>>>(a);
-    else if (pieces <= 8192) categorical_kernel<T, 1024, 8><<<rows, 1024, 0, stream>>>(a);
-    else if (pieces <= 16384) categorical_kernel<T, 1024, 16><<<rows, 1024, 0, stream>>>(a);
-    else categorical_kernel<T, 1024, 0><<<rows, 1024, 0, stream>>>(a);
+    // (past one row of the grid the rows go on in the next)
+    auto go = [&](auto* kernel, int tpr) {
+        const int threads = tpr < 256 ? 256 : tpr;
+        const int64_t blocks = (a.M * tpr + threads - 1) / threads;
+        const unsigned row = groups_of(blocks, threads);
+        kernel<<<dim3(row, (unsigned)((blocks + row - 1) / row)), threads, 0, stream>>>(a);
+    };
+    if (pieces <= 32) go(categorical_kernel<T, 16, 2>, 16);
+    else if (pieces <= 64) go(categorical_kernel<T, 32, 2>, 32);
+    else if (pieces <= 256) go(categorical_kernel<T, 64, 4>, 64);
+    else if (pieces <= 1024) go(categorical_kernel<T, 256, 4>, 256);
+    else if (pieces <= 2048) go(categorical_kernel<T, 256, 16>, 256);
+    else if (pieces <= 8192) go(categorical_kernel<T, 1024, 8>, 1024);
+    else if (pieces <= 16384) go(categorical_kernel<T, 1024, 16>, 1024);
+    else go(categorical_kernel<T, 1024, 0>, 1024);
     return hipGetLastError();
 }
 

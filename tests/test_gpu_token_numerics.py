@@ -305,3 +305,28 @@ def test_a_single_row_of_a_larger_tensor(s, dtype):
     dy = rand(1, N, t=t)
     for a, b in zip(s.linear_grad(dy, row, w, act="silu", pre=pre), s.linear_grad(dy, one, w, act="silu", pre=pre)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("M,V", [((1 << 21) + 9, 7), (4_000_003, 2), ((1 << 26) + 17, 1), ((1 << 20) + 3, 1040)])
+def test_likelihood_of_very_many_rows(s, M, V):
+    torch = _torch()
+    say("likelihood", M, V)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    dtype = torch.bfloat16 if V > 1000 else torch.float32
+    z = torch.randn(M, V, device="cuda", generator=g).to(dtype)
+    t = torch.randint(-1, V, (M,), device="cuda", generator=g)
+    nll, total, dz = s.categorical(z, t, grad=True, scale=0.25)
+    there = t >= 0
+    for at in list(range(0, M, M // 5 + 1)) + [M - 30]:  # some rows of each part, and the last ones
+        r = slice(at, at + 1000)
+        zd, seen = z[r].double(), there[r]
+        lse = torch.logsumexp(zd, 1)
+        ref = torch.where(seen, lse - zd.gather(1, t[r].clamp(min=0)[:, None])[:, 0], torch.zeros_like(lse))
+        # (8 roundings of values of size |z|, |lse| < 16; sums of up to 1040 exponentials as a tree)
+        assert ((nll[r].double() - ref).abs() <= 200 * U).all()
+        p = torch.exp(zd - lse[:, None])
+        p.scatter_add_(1, t[r].clamp(min=0)[:, None], -torch.ones_like(p[:, :1]))
+        p *= 0.25 * seen[:, None]
+        assert ((dz[r].double() - p).abs() <= 100 * U + (p.abs() * 2.0 ** -8 if V > 1000 else 0)).all()
+    want = float(nll.sum(dtype=torch.float64))
+    assert abs(float(total) - want) <= 1e-9 * abs(want) + 1e-9
