@@ -20,6 +20,8 @@
  *     are the fast case).  Sizes are >= 0 and below 2^31; strides of the linear
  *     layer's and the gated block's matrices below 2^23 (NUTS_EUNSUPPORTED);
  *     nothing is done where an output is empty, and an empty sum is zero.
+ *   - A scale is taken in fp32: zero, or a magnitude of 2^-126 to the largest fp32
+ *     value (NUTS_EINVAL otherwise).
  *   - Outputs do not overlap inputs, except where stated.
  *   - Arithmetic is fp32 or wider, rounded once on output.  bf16 matrix
  *     products run on the bf16 matrix cores with fp32 sums; fp32 ones either on

@@ -52,7 +52,10 @@ struct Check {
     }
     void scale(double s)
     {
-        if (!(s - s == 0.0)) refuse(NUTS_EINVAL, "scale must be finite");
+        // (the kernels take it in fp32)
+        const double size = s < 0.0 ? -s : s;
+        if (!(size == 0.0 || (size >= 0x1p-126 && size <= (double)__FLT_MAX__)))
+            refuse(NUTS_EINVAL, "scale must be zero or a finite, normal fp32 value (got %g)", s);
     }
     // A buffer of `elems` elements of `bytes` each; needed unless it is empty.
     void buffer(const char* name, const void* p, int64_t elems, size_t bytes, bool needed = true)

@@ -330,3 +330,20 @@ def test_likelihood_of_very_many_rows(s, M, V):
         assert ((dz[r].double() - p).abs() <= 100 * U + (p.abs() * 2.0 ** -8 if V > 1000 else 0)).all()
     want = float(nll.sum(dtype=torch.float64))
     assert abs(float(total) - want) <= 1e-9 * abs(want) + 1e-9
+
+
+def test_scale_in_every_call(s):
+    import paper_1912_11554_amd as nuts
+    torch = _torch()
+    say("scales")
+    ids, z = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, 4, device="cuda")
+    for scale in (1e39, 1e-40):
+        for call in (lambda: s.embedding(ids, z, scale=scale), lambda: s.embedding_grad(ids, z, 2, scale=scale),
+                     lambda: s.categorical(z, ids, grad=True, scale=scale)):
+            with pytest.raises(nuts.NutsError) as e:
+                call()
+            assert e.value.code == nuts.NUTS_EINVAL and "scale" in str(e.value)
+    big = torch.finfo(torch.float32).max
+    assert torch.equal(s.embedding(ids, z, scale=big), z[:3])
+    one = torch.full((1, 4), 2.0 ** 100, device="cuda")
+    assert torch.equal(s.embedding(ids[:1], one, scale=2.0 ** -126), one * 2.0 ** -126)

@@ -86,3 +86,20 @@ def test_rounding_is_a_gradients_choice():
         assert L.nuts_linear_workspace(ctypes.byref(a)) == nuts.NUTS_EINVAL
     a = ops._LinearGrad(2, silu + 512, 64, 64, 64, p, 64, p, 64, p, 64, p, p, 64, None, 0, None)
     assert L.nuts_linear_grad_workspace(ctypes.byref(a)) == nuts.NUTS_EINVAL
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e300, 3.4028236e38, 1e-46, -1e-39, float("inf"), float("-inf"), float("nan")])
+def test_scales_outside_fp32_are_refused(scale):
+    # (in fp32 they are an infinity, whose product with a zero is no zero, or lose their digits)
+    L = nuts.load_library()
+    p = 1 << 20
+    a = ops._EmbeddingGrad(1, 0, 100, 9, 65, p, p, 65, scale, p, 65)
+    assert L.nuts_embedding_grad_workspace(ctypes.byref(a)) == nuts.NUTS_EINVAL
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 2.0 ** -126, -3.4028234663852886e38, 1.0 / 3])
+def test_scales_of_fp32_are_taken(scale):
+    L = nuts.load_library()
+    p = 1 << 20
+    a = ops._EmbeddingGrad(1, 0, 100, 9, 65, p, p, 65, scale, p, 65)
+    assert L.nuts_embedding_grad_workspace(ctypes.byref(a)) > 0
