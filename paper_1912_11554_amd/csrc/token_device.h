@@ -86,10 +86,22 @@ __device__ __forceinline__ void store_f32(void* p, int dtype, int64_t i, float v
     else ((float*)p)[i] = v;
 }
 
-// act(z).  The logistic function through exp2 and the reciprocal of the fp32
-// units: exp(-z) overflows to infinity below z = -88, whose reciprocal is the
-// limit 0; z = -infinity gives silu 0, its limit.
-__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// exp(x + rest), |rest| far below |x|, as 2^t: what rounding takes off t = x log2(e)
+// goes into a factor 1 + d ln 2.  Left to itself that rounding is a relative error of
+// |x| 2^-24.
+__device__ __forceinline__ float exp_f32(float x, float rest = 0.0f)
+{
+    constexpr float log2e = 0x1.715476p+0f, log2e_low = 0x1.4ae0cp-26f, ln2 = 0x1.62e43p-1f;  // log2(e), in two parts
+    const float t = x * log2e;
+    const float d = fmaf(x, log2e_low, fmaf(rest, log2e, fmaf(x, log2e, -t)));
+    const float e = __builtin_amdgcn_exp2f(t);
+    return fabsf(t) < 126.0f ? fmaf(e, d * ln2, e) : e;  // (past that e may be 0, an infinity or NaN)
+}
+
+// act(z).  The logistic function with the reciprocal of the fp32 units: exp(-z)
+// overflows to infinity below z = -88, whose reciprocal is the limit 0; z =
+// -infinity gives silu 0, its limit.
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + exp_f32(-z)); }
 
 __device__ __forceinline__ float activate(float z, int act)
 {
@@ -126,7 +138,8 @@ __device__ __forceinline__ void activate_slope(float z, int act, float* a, float
     }
     case NUTS_ACT_GELU: {
         const float cdf = 0.5f * erfcf(-z * 0.70710678118654752f);
-        const float pdf = 0.39894228040143268f * __expf(-0.5f * z * z);
+        const float square = z * z;
+        const float pdf = 0.39894228040143268f * exp_f32(-0.5f * square, -0.5f * fmaf(z, z, -square));
         *a = z == -__builtin_inff() ? 0.0f : z * cdf;
         *slope = cdf + (fabsf(z) == __builtin_inff() ? 0.0f : z * pdf);
         break;

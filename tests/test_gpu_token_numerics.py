@@ -30,13 +30,18 @@ def _gen(seed):
     return lambda *q, std=1.0, t=torch.float32: (torch.randn(*q, device="cuda", generator=g) * std).to(t)
 
 
+def _cdf(z):
+    """The normal distribution function (torch's own cancels below -6)."""
+    return 0.5 * _torch().special.erfc(-z * 0.5 ** 0.5)
+
+
 def _act(z, kind):
     """act(z) and its slope, in z's 64 bits."""
     torch = _torch()
     if kind == "none":
         return z, torch.ones_like(z)
     if kind == "gelu":
-        cdf = torch.special.ndtr(z)
+        cdf = _cdf(z)
         return z * cdf, cdf + z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
     p, q = torch.special.expit(z), torch.special.expit(-z)
     return (p, p * q) if kind == "sigmoid" else (z * p, p + z * p * q)
@@ -347,3 +352,56 @@ def test_scale_in_every_call(s):
     assert torch.equal(s.embedding(ids, z, scale=big), z[:3])
     one = torch.full((1, 4), 2.0 ** 100, device="cuda")
     assert torch.equal(s.embedding(ids[:1], one, scale=2.0 ** -126), one * 2.0 ** -126)
+
+
+# --------------------------------------------------------------------------
+# Activations far from zero, relative to their own size.  In units of u = 2^-24
+# an exponential is off by 4 (the unit's last place, the correction's rounding and
+# product), a reciprocal by 2, every sum and product by 1.
+
+def _points():
+    torch = _torch()
+    return torch.cat([torch.linspace(-80, 80, 40001), torch.linspace(-4, 4, 4001)]).cuda()
+
+
+def _activated(s, z, act):
+    """act(z) and its slope by the kernels: z as a layer of one input, and the
+    gradient of its weights."""
+    torch = _torch()
+    one = torch.ones(1, 1, device="cuda")
+    y, pre = s.linear(one, z[:, None], act=act, save=True)
+    assert torch.equal(pre[0], z)
+    dw = s.linear_grad(torch.ones_like(y), one, z[:, None], act=act, pre=pre, dx=False, bias=False)[1]
+    return y[0].double(), dw[:, 0].double()
+
+
+@pytest.mark.parametrize("act", ["sigmoid", "silu"])
+def test_relative_error_of_the_logistic_function(s, act):
+    torch = _torch()
+    say("logistic", act)
+    z = _points()
+    zd = z.double()
+    y, slope = _activated(s, z, act)
+    ref, dref = _act(zd, act)
+    assert ((y - ref).abs() <= 9 * U * ref.abs()).all()
+    if act == "silu":  # (for z < 0; its two parts cancel near -1.28)
+        p, q = torch.special.expit(zd), torch.special.expit(-zd)
+        low = z < 0
+        assert ((slope - dref).abs() <= 20 * U * (p + zd.abs() * p * q))[low].all()
+    # the same function in the tiles' epilogue
+    x = torch.ones(70, 1, device="cuda")
+    assert torch.equal(s.linear(x, z[:, None], act=act), y.float().expand(70, -1))
+
+
+def test_relative_error_of_the_gelu_slope(s):
+    # the normal density takes 16 u; the distribution function's argument is rounded,
+    # which z^2 u of its value goes with
+    say("gelu slope")
+    z = _points()
+    z = z[z.abs() < 9]
+    zd = z.double()
+    torch = _torch()
+    cdf, pdf = _cdf(zd), torch.exp(-zd * zd / 2) / (2 * torch.pi) ** 0.5
+    slope = _activated(s, z, "gelu")[1]
+    tol = (16 + 2 * zd * zd) * U * cdf + 16 * U * zd.abs() * pdf
+    assert ((slope - (cdf + zd * pdf)).abs() <= tol).all()
