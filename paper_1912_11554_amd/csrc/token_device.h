@@ -114,6 +114,15 @@ __device__ __forceinline__ float activate(float z, int act)
     }
 }
 
+// p = logistic(z) and p (1 - p).  1 - p is logistic(-z) and taken as such: near p = 1
+// the difference has few digits, or none.
+__device__ __forceinline__ void logistic_slope(float z, float* p, float* pq)
+{
+    const float e = exp_f32(-fabsf(z)), d = __builtin_amdgcn_rcpf(1.0f + e);
+    *p = z < 0.0f ? e * d : d;
+    *pq = e * d * d;
+}
+
 // act(z) and act'(z).
 __device__ __forceinline__ void activate_slope(float z, int act, float* a, float* slope)
 {
@@ -123,17 +132,15 @@ __device__ __forceinline__ void activate_slope(float z, int act, float* a, float
         *slope = z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
         break;
     case NUTS_ACT_SIGMOID: {
-        const float p = logistic(z);
-        *a = p;
-        *slope = p * (1.0f - p);
+        logistic_slope(z, a, slope);
         break;
     }
     case NUTS_ACT_SILU: {
         // an infinite z takes the limits: 0 and 0, or z and 1
-        const float p = logistic(z);
-        const float q = p * (1.0f - p);
-        *a = activate(z, act);
-        *slope = p + (fabsf(z) == __builtin_inff() ? 0.0f : z * q);
+        float p, pq;
+        logistic_slope(z, &p, &pq);
+        *a = z == -__builtin_inff() ? 0.0f : z * p;
+        *slope = p + (fabsf(z) == __builtin_inff() ? 0.0f : z * pq);
         break;
     }
     case NUTS_ACT_GELU: {

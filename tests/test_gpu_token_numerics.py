@@ -405,3 +405,28 @@ def test_relative_error_of_the_gelu_slope(s):
     slope = _activated(s, z, "gelu")[1]
     tol = (16 + 2 * zd * zd) * U * cdf + 16 * U * zd.abs() * pdf
     assert ((slope - (cdf + zd * pdf)).abs() <= tol).all()
+
+
+def _slopes(s, z, act):
+    """act's slope by the kernels, as the bias gradient of one row: no product
+    (which would take values to multiples of 2^-133) is in the way."""
+    torch = _torch()
+    one = torch.ones(1, 1, device="cuda")
+    _, pre = s.linear(one, z[:, None], act=act, save=True)
+    return s.linear_grad(torch.ones_like(pre), one, z[:, None], act=act, pre=pre, dx=False, dw=False)[2].double()
+
+
+def test_relative_error_of_the_logistic_slope(s):
+    # p (1 - p): an exponential, and a reciprocal's square; silu's slope by it on both sides
+    torch = _torch()
+    say("logistic slope")
+    z = _points()
+    p, q = torch.special.expit(z.double()), torch.special.expit(-z.double())
+    assert ((_slopes(s, z, "sigmoid") - p * q).abs() <= 16 * U * p * q).all()
+    zd = z.double()
+    assert ((_slopes(s, z, "silu") - (p + zd * p * q)).abs() <= 20 * U * (p + zd.abs() * p * q)).all()
+    # NaN and infinities
+    z = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda")
+    for act, want in (("sigmoid", [0.0, 0.0]), ("silu", [1.0, 0.0])):
+        slope = _slopes(s, z, act)
+        assert torch.isnan(slope[0]) and slope[1:].tolist() == want
