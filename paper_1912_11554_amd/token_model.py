@@ -73,7 +73,8 @@ class TokenModel:
     def leapfrog(self, w, p, grad, step_size, steps):
         """``steps`` leapfrog steps from positions w, momenta p and the
         gradient at w (none is changed).  Returns positions, momenta, U and the
-        gradient at the end."""
+        gradient at the end.  Positions are float32 (see ``sample``)."""
+        _need_f32(w)
         w = {k: v.clone() for k, v in w.items()}
         p = {k: v.clone() for k, v in p.items()}
         U = None
@@ -88,7 +89,12 @@ class TokenModel:
 
     def sample(self, w, *, step_size, steps, num_samples, seed=0):
         """Hamiltonian Monte Carlo from w with unit masses.  Returns the last
-        position and, per sample, U and whether the proposal was taken."""
+        position and, per sample, U and whether the proposal was taken.
+
+        Positions are float32: rounded to bfloat16 at every step they would
+        neither run backwards nor preserve volume, which the acceptance
+        probability relies on (``potential`` and ``potential_grad`` take both)."""
+        _need_f32(w)
         g = torch.Generator(device=self.tokens.device).manual_seed(seed)
         U, grad = self.potential_grad(w)
         trace = []
@@ -101,6 +107,12 @@ class TokenModel:
                 w, U, grad = w2, U2, grad2
             trace.append((float(U), take))
         return w, trace
+
+
+def _need_f32(w):
+    for k, v in w.items():
+        if v.dtype != torch.float32:
+            raise TypeError(f"{k}: positions of a trajectory must be float32, got {v.dtype}")
 
 
 def kinetic(p):
