@@ -75,6 +75,8 @@ class TokenModel:
         gradient at w (none is changed).  Returns positions, momenta, U and the
         gradient at the end.  Positions are float32 (see ``sample``)."""
         _need_f32(w)
+        if steps < 1:
+            raise ValueError(f"a trajectory has at least one step, got {steps}")
         w = {k: v.clone() for k, v in w.items()}
         p = {k: v.clone() for k, v in p.items()}
         U = None

@@ -21,3 +21,11 @@ def test_trajectories_in_bf16_are_refused():
     mixed["head"] = mixed["head"].double()
     with pytest.raises(TypeError, match="head"):
         m.sample(mixed, step_size=0.1, steps=2, num_samples=1)
+
+
+@pytest.mark.parametrize("steps", [0, -1])
+def test_trajectories_of_no_steps_are_refused(steps):
+    m = _model()
+    w = m.init()
+    with pytest.raises(ValueError, match="at least one step"):
+        m.leapfrog(w, w, w, 0.1, steps)
