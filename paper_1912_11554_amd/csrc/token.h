@@ -59,6 +59,39 @@ struct Product {
     Term terms[2][kMaxTerms];
     Epilogue epi[2];
 };
+constexpr int kStep = 64;  // k of a stage (32 for fp32)
+constexpr int kMaxSlices = 32;
+
+// Tiles and slices.  A unit has places for one workgroup of 256 x 256 tiles, two
+// of 128 x 128, four of 64 x 64.  The largest tile that fills three quarters of
+// the places is taken, the sum in slices where there are fewer tiles than places.
+// The slices' sums are written, read and added, 7 us at 1000 x 1027 and 14 us at 777
+// x 3592: a slice has 512 k at least (256 of the small tiles'), and small tiles one
+// for each unit are not sliced.  fp32 at 1000 x 1027 x 513: 22 us in 64 x 64 tiles, 24
+// in two slices, 28 in 128 x 128 tiles and two slices; 777 x 3592 x 640: 34, 44 and 41
+// us; 777 x 640 x 3592: 94 us whole, 48 in four slices, 64 in 128 x 128 tiles and four.
+struct Plan {
+    int tile, slices;
+};
+inline int64_t steps_of(const Product& p)
+{
+    const int ks = p.dtype == NUTS_F32 ? 32 : kStep;
+    return (p.K + ks - 1) / ks;
+}
+inline Plan plan_product(const Product& p, int num_cu)
+{
+    for (int tile = p.staged ? 128 : 256;; tile /= 2) {
+        const int64_t tiles = ((p.M + tile - 1) / tile) * ((p.N * (p.gated ? 2 : 1) + tile - 1) / tile) * p.sets;
+        const int64_t places = (int64_t)num_cu * (tile == 256 ? 1 : tile == 128 ? 2 : 4);
+        int64_t s = tile == 256 || tiles >= (tile == 64 ? num_cu : places) ? 1 : places / tiles;
+        const int64_t most = p.K * p.nterms / (tile == 64 ? 256 : 512);
+        if (s > most) s = most;
+        if (s > kMaxSlices) s = kMaxSlices;
+        if (s < 1) s = 1;
+        if (tile == 64 || tiles * s >= places * 3 / 4) return {tile, (int)s};
+    }
+}
+
 // fp32 partial sums that the product needs (bytes), by its sizes alone.
 size_t product_workspace(const Product& p, int num_cu);
 hipError_t launch_product(const Product& p, float* partials, int num_cu, hipStream_t stream);
