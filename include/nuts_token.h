@@ -18,14 +18,15 @@
  *     elements, ld >= the row's length; any alignment of the element type is
  *     taken (bf16 rows of a whole multiple of 8 elements on 16-byte boundaries
  *     are the fast case).  Sizes are >= 0 and below 2^31; strides of the linear
- *     layer's and the gated block's matrices below 2^23 (NUTS_EUNSUPPORTED);
+ *     layer's and the gated block's matrices below 2^23, and of any two of the three
+ *     sizes of a product, (one / 64) (other / 32) below 2^24 (NUTS_EUNSUPPORTED);
  *     nothing is done where an output is empty, and an empty sum is zero.
  *   - A scale is taken in fp32: zero, or a magnitude of 2^-126 to the largest fp32
  *     value (NUTS_EINVAL otherwise).
  *   - Outputs do not overlap inputs, except where stated.
  *   - Arithmetic is fp32 or wider, rounded once on output.  bf16 matrix
  *     products run on the bf16 matrix cores with fp32 sums; fp32 ones either on
- *     the fp32 matrix cores (up to 64 rows of x) or as three bf16 parts a factor
+ *     the fp32 matrix cores (forward, few rows of x) or as three bf16 parts a factor
  *     (products of relative size 2^-22 and below left out; a factor to multiples
  *     of 2^-133, so below 2^-110 it has fewer digits and below 2^-133 it is zero).
  *     Infinities and NaN come out as in fp32 products of these factors.

@@ -3,9 +3,9 @@
 // Both move memory and compute next to nothing.  The gradient sorts the
 // positions by token (a stable radix sort, least digit first: the order of a
 // token's positions, and so its sum, is fixed), sums runs of equal tokens in
-// chunks of sorted positions, so that a token that fills half a batch is spread
-// over the device like any other, and joins the chunks' sums while it writes the
-// table.
+// chunks of sorted positions, so that a token that fills half a batch is read by the
+// whole device, and joins the chunks' sums while it writes the table: a token's in
+// the threads of its row, one after the other.
 #include "token.h"
 #include "token_device.h"
 
@@ -150,7 +150,7 @@ struct Sorted {
 // pass: a wave counts its own run's digits, the counts are summed in (digit, wave)
 // order, and a wave's lanes take their places in order of the run: lanes with one
 // digit find each other by a ballot a bit.  Bound by the latency of the chain of
-// LDS accesses: 5000 positions of 20,011 tokens took 16 us.
+// LDS accesses: 1000, 2000 and 4000 positions of 20,011 tokens take 6, 8 and 12 us.
 __global__ __launch_bounds__(64 * kSmallWaves) void small_sort_kernel(const int64_t* ids, int N, int64_t V, int bits,
                                                                       Sorted out)
 {
@@ -247,8 +247,8 @@ static_assert((1 << kSmallBits) * kSmallWaves == 4 * 64 * kSmallWaves, "four cou
 
 // Many positions: workgroups of consecutive positions, a pass a digit of up to
 // 9 bits: counts, then every workgroup's place for each digit from all counts.
-// Bound by latency (32,768 positions move 2 MB a pass): a pass takes 10 us of
-// counting, with marking 64,000 tokens absent in the first, and 14 us of placing, of
+// Bound by latency (32,768 positions move 2 MB a pass): a pass takes 5 us of
+// counting, with marking 64,000 tokens absent in the first, and 7 us of placing, of
 // which reading the other workgroups' counts is the most.  256 workgroups at most keep
 // those counts few; digits of 9 bits sort 64,000 tokens in two passes.
 constexpr int kSortGroups = 256;
@@ -449,7 +449,10 @@ __global__ __launch_bounds__(256) void chunk_sum_kernel(nuts_embedding_grad_args
         chunk_sum<T, W, PAST>(a, s, partial, b / cols * (256 / tx) + threadIdx.x / tx, run_column<W>(b % cols, tx, a.D));
 }
 
-// The rows of tokens that no chunk finished: zeros, or the partial rows' sum.
+// The rows of tokens that no chunk finished: zeros, or the partial rows' sum.  A token
+// of n positions is a chain of n / 32 additions here: 65,536 positions of 100 tokens,
+// 1024 bf16 wide, take 133 us where a third of them hold one token, 53 us where all
+// are as frequent.
 constexpr int kTableRows = 4;  // of a thread
 template <typename T, int W, bool PAST>
 __global__ __launch_bounds__(256) void table_kernel(nuts_embedding_grad_args a, Sorted s, const float* partial, int tx,

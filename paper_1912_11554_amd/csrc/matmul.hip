@@ -323,10 +323,11 @@ __device__ __forceinline__ int small_end(const ConstArgs& p, Run run)
 // 2 M N K operations on matrix cores.  A 256 x 256 tile by 8 waves (128 x 64 each,
 // 128 fp32 sums a lane) takes 64 KB for 64 k; the copies alone need 0.95 us a stage,
 // the reads of LDS alone 0.42, the products without copies 0.8 to 0.9: the copies
-// bound it, then the clock that the products leave.  Normally distributed inputs:
-// 8192 x 2048 x 8192 274 us (1.00 PFLOP/s), its gradients 288 and 267 us; the gated
-// pair 8192 x 24,576 x 4096 1340 us (1.23); gradients of 4096 x 8192 x 4096, two terms
-// or two sets, 457 and 494 us (1.20 and 1.11).  The epilogue adds 8 us for each
+// bound it, then the clock that the products leave.  Normally distributed inputs, on
+// several cards: 8192 x 2048 x 8192 274 to 286 us (1.00 to 0.96 PFLOP/s), its gradients
+// 288 to 296 and 267 to 270 us; the gated pair 8192 x 24,576 x 4096 1340 to 1400 us
+// (1.23 to 1.18); gradients of 4096 x 8192 x 4096, two terms or two sets of two parts,
+// 906 to 914 and 944 to 950 us (1.21 and 1.16).  The epilogue adds 8 us for each
 // round of tiles, the rate at which memory takes the results.  128 x 128 and 64 x 64
 // tiles are for products with few tiles.
 // Tried, and slower or equal: 32 k a stage with three to five stages (7 to 10%
@@ -979,15 +980,15 @@ hipError_t launch_few_rows(const FewRows& p, hipStream_t stream)
 // x 8 columns: 4 waves take ROWS / 4 rows each, all of them in flight, a
 // lane eight columns; with dbias, sums over its rows by wave, then over the
 // waves, and a second kernel adds the workgroups' sums.  Bound by memory: the gated
-// block's 4096 x 8192 bf16 (dy, both fp32 pre-activations, dg and du: 470 MB) 110 us (4.3
-// TB/s); sums alone of 8192 x 2048 bf16 11 and 5 us.
+// block's 4096 x 8192 bf16 (dy, both fp32 pre-activations, dg and du in two parts: 604 MB)
+// 117 to 122 us (5.0 to 5.2 TB/s); sums alone of 8192 x 2048 bf16 12 and 5 us.
 namespace {
 
 // Rows of a workgroup: four, a row a wave; sixteen with sums, a quarter of them to
 // add again, where there are elements for it.  silu and dbias alone, bf16 (us,
 // sixteen in parentheses): 1024 x 1024 6.7 (7.5), 777 x 3592 8.7 (9.0), 2048 x 2048 11.0
-// (9.5), 8192 x 4096 47 (40).  With dx after it and no dbias: 8192 x 4096 60 (66), the
-// gated block's 110 (117).
+// (9.5), 8192 x 4096 47 (40).  With dx after it and no dbias, one part: 8192 x 4096 60
+// (66), the gated block's 110 (117).
 int64_t slope_rows(int64_t M, int64_t N, bool sums) { return sums && M * N >= (int64_t)1 << 22 ? 16 : 4; }
 
 // (Past one row of the grid the work goes on in the next: a loop over it costs 7%, this 2.)

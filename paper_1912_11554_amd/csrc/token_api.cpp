@@ -172,8 +172,8 @@ struct Backward {
 // A bf16 dz rounded once adds as much error to its products as their own rounding
 // does (2.3e-3 of their norm in all, where one rounding leaves 1.7e-3).  So it is kept
 // in two bf16 matrices (16 bits), twice the products, unless the caller asks for one
-// (linear layer and gated block, one part and two, us: 128 x 1024 x 1024 16.4 and 19.6,
-// 19.7 and 26.5; 1024^3 27 and 46, 41 and 60).
+// (linear layer and gated block, one part and two, us: 128 x 1024 x 1024 22 and 23, 24
+// and 28; 1024^3 28 and 45, 40 and 61; 8192 x 2048 x 8192 540 and 944, 958 and 1801).
 const void* part_of(const void* dz, int part, int64_t rest)
 {
     return dz ? (const char*)dz + (part ? rest * 2 : 0) : nullptr;
